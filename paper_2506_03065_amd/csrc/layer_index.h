@@ -55,6 +55,9 @@ constexpr ChunkRange chunks_of(const RowChunks& c, const int g) {
   return {c0, behind + 1 + (c.first > 0 ? 1 : 0) < c.groups ? c0 + c.group_chunks : c.per_entry};
 }
 
+// The row `step` behind `row` in a chunk that ends at `end`, or `end` if there is none (row + step may itself be past 2^31).
+constexpr int row_behind(int row, int step, int end) { return end - row > step ? row + step : end; }
+
 // Lanes of a row: up to 1,024 channels a work-group of 256 takes several rows at once, a row to 16, 32 or 64 lanes, so that its sums
 // need no barrier; above (0) it takes one row.  Pieces of 8 channels that a thread holds.  (A work-group a row at any width, 8
 // channels a thread: 123,375 x 96 fp32: forward 66 us against 33, backward 356 against 63; 75,600 x 512 bf16: 63 against 61, and 200

@@ -185,17 +185,19 @@ __global__ void __launch_bounds__(NJ == 1 || LANES ? 256 : 512) norm_forward_ker
       if (has_y) y_next[j].load(row_of<const __bf16>(p.y, ch.b, row) + ln.at[j]);
     }
   };
-  const int row0 = ch.row0 + (LANES ? (int)threadIdx.x / LANES : 0);
+  // a row at a time: row + 1 is at most ch.row1
+  auto behind = [&](int row, int step) { return LANES ? row_behind(row, step, ch.row1) : row + step; };
+  const int row0 = behind(ch.row0, LANES ? (int)threadIdx.x / LANES : 0);
   if (row0 < ch.row1) request(row0);
   if (!LANES) clear_slots(&slots[0][0][0], sizeof(slots) / sizeof(slots[0][0][0]));
-  for (int row = row0; row < ch.row1; row += ROWS) {
+  for (int row = row0; row < ch.row1; row = behind(row, ROWS)) {
     f32x8 x[NJ], y[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       x[j] = x_next[j].get();
       y[j] = y_next[j].get();
     }
-    if (row + ROWS < ch.row1) request(row + ROWS);
+    if (behind(row, ROWS) < ch.row1) request(behind(row, ROWS));
     Slot<NJ> (*slot)[2] = slots[row & 1];
     if (has_y) {
       Stats st = {0.f, 1.f};
@@ -296,10 +298,11 @@ __global__ void __launch_bounds__(NJ == 1 || LANES ? 256 : 512) norm_backward_ke
       if (has_y) y_next[j].load(row_of<const __bf16>(p.y, ch.b, row) + ln.at[j]);
     }
   };
-  const int row0 = ch.row0 + (LANES ? (int)threadIdx.x / LANES : 0);
+  auto behind = [&](int row, int step) { return LANES ? row_behind(row, step, ch.row1) : row + step; };
+  const int row0 = behind(ch.row0, LANES ? (int)threadIdx.x / LANES : 0);
   if (!kLean && row0 < ch.row1) request(row0);
   if (!LANES) clear_slots(&slots[0][0][0], sizeof(slots) / sizeof(slots[0][0][0]));
-  for (int row = row0; row < ch.row1; row += ROWS) {
+  for (int row = row0; row < ch.row1; row = behind(row, ROWS)) {
     f32x8 x[NJ], y[NJ], dh[NJ], dx[NJ];
     if (kLean) request(row);
 #pragma unroll
@@ -309,7 +312,7 @@ __global__ void __launch_bounds__(NJ == 1 || LANES ? 256 : 512) norm_backward_ke
       dh[j] = dh_next[j].get();
       dx[j] = up_next[j].get();
     }
-    if (!kLean && row + ROWS < ch.row1) request(row + ROWS);
+    if (!kLean && behind(row, ROWS) < ch.row1) request(behind(row, ROWS));
     Slot<NJ> (*slot)[2] = slots[row & 1];
     // the statistics of both rows in one go
     Part px = {0.f, 0.f}, py = {0.f, 0.f};
