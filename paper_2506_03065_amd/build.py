@@ -11,6 +11,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -27,16 +29,22 @@ def hipcc_path() -> str:
     raise RuntimeError("hipcc not found; the library cannot be built")
 
 
-def build_library(verbose: bool = True) -> str:
-    cmd = [hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-x", "hip",
-           # NaNs need no special care in fmax chains (infinities stay honoured: masks use -inf)
-           "-fno-honor-nans",
+# What the calls of these say about infinities and NaN holds: their compiler may not assume that there are none.
+HONOR_NANS = ("norm_kernels.hip", "rope_kernels.hip", "blockscale_kernels.hip", "layer_api.cpp")
+
+
+def compile_command(source: str, out: str) -> list[str]:
+    cmd = [hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
            # packed fp32 VALU forms are kept out of the generated code on purpose
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-o", LIB_PATH]
+    if source not in HONOR_NANS:
+        # attention: NaNs need no special care in fmax chains (infinities stay honoured: masks use -inf)
+        cmd.append("-fno-honor-nans")
+    return cmd + ["-c", os.path.join(CSRC, source), "-o", out]
+
+
+def _run(cmd: list[str], verbose: bool) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -44,6 +52,14 @@ def build_library(verbose: bool = True) -> str:
     err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
     if res.returncode != 0:
         raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
+    return err
+
+
+def build_library(verbose: bool = True) -> str:
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(4) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        err = "".join(pool.map(lambda s, o: _run(compile_command(s, o), verbose), SOURCES, objects))
+        err += _run([hipcc_path(), "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB_PATH], verbose)
     if verbose and err.strip():
         print(err, file=sys.stderr)
     return LIB_PATH
