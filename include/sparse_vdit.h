@@ -565,7 +565,8 @@ svd_status svd_residual_norm_backward(const svd_norm_desc* desc, const svd_norm_
  * channel pairs the first pairs_t turn with the frame, the next pairs_h with the
  * row, the next pairs_w with the column, the rest not at all; tokens outside the
  * video do not turn.  Pair p: channels (2p, 2p + 1) or (p, p + D/2).
- * (a, b) -> (a cos - b sin, a sin + b cos). */
+ * (a, b) -> (a cos - b sin, a sin + b cos); with a sin of 0, (a cos, b cos): what
+ * does not turn keeps its bits, whatever stands beside it. */
 enum { SVD_ROPE_ADJACENT = 0, SVD_ROPE_HALVES = 1 };
 typedef struct {
   int32_t first, frames, height, width;

@@ -86,8 +86,11 @@ __device__ __forceinline__ f32x8 turn(const f32x8 v, const Angles& a, const floa
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float x = v[P::first(i)], y = v[P::second(i)], s = sign * a.sin[i];
-    o[P::first(i)] = x * a.cos[i] - y * s;
-    o[P::second(i)] = x * s + y * a.cos[i];
+    // What does not turn keeps its bits, zeros' signs too, whatever stands beside it: 1 * 0 is subtracted, -1 * 0 added.
+    const bool turns = s != 0.f;
+    const float one = __builtin_copysignf(1.f, s), xs = turns ? x : -one, ys = turns ? y : one;
+    o[P::first(i)] = __builtin_fmaf(x, a.cos[i], -(ys * s));
+    o[P::second(i)] = __builtin_fmaf(xs, s, y * a.cos[i]);
   }
   return o;
 }

@@ -119,3 +119,25 @@ def test_rows_of_the_rotary_gradients(pairing):
         assert torch.isnan(got[b, h, l]).all()
         got[b, h, l] = clean[b, h, l]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("pairing", ["adjacent", "halves"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_what_does_not_turn_keeps_its_bits(pairing, D):
+    """Tokens outside the video, pairs without an axis and position 0: infinities, zeros of either sign and NaN beside them."""
+    desc = svd.rope_desc(3, 2, 2, (8, 4, 4), first=5, pairing=pairing)
+    table = torch.empty(svd.svd_rope_table_bytes(desc) // 8, 2, device=DEV)
+    svd.svd_rope_table(desc, table)
+    values = torch.tensor([1.5, INF, -0.0, 0.0, -INF, 3.0, NAN, -2.0], device=DEV)
+    pick = torch.randint(0, 8, (2, 2, 40, D), device=DEV, generator=torch.Generator(device=DEV).manual_seed(D))
+    x = values[pick].to(BF)
+    pair = torch.arange(D, device=DEV) % (D // 2) if pairing == "halves" else torch.arange(D, device=DEV) // 2
+    still = torch.ones(40, D, dtype=torch.bool, device=DEV)
+    still[6:17] = pair >= 16                # the video but its first token; pairs from the 16th on have no axis
+    out, back = torch.empty_like(x), torch.empty_like(x)
+    svd.svd_rope_forward(desc, table, [(x, out)])
+    svd.svd_rope_backward(desc, table, [(None, x, back)])
+    number = still & ~torch.isnan(x)
+    for o in (out, back):
+        assert torch.equal(o.view(torch.int16)[number], x.view(torch.int16)[number])
+        assert torch.isnan(o[still & torch.isnan(x)]).all()
