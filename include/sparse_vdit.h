@@ -78,7 +78,7 @@ typedef struct {
   int32_t B, H, L, D;                     /* D in {64, 128} */
   int64_t stride_b, stride_h, stride_l;   /* in elements; the D axis has stride 1 */
 } svd_tensor_desc;
-/* Size limits (SVD_ERR_UNSUPPORTED beyond them): the rows of one head span less
+/* Size limits of the attention's calls (SVD_ERR_UNSUPPORTED beyond them): the rows of one head span less
  * than 4 GiB (L * stride_l * 2 < 2^32), L < 2^24, and a row stride below 16 MiB. */
 
 /* Parameters of one head (pattern_params is an array of H of these).  Only the
@@ -597,7 +597,9 @@ typedef struct {
   const float *weight, *bias;
 } svd_rope_tensor;
 /* 1 or 2 tensors of the same B, L and D in one launch (their head counts may
- * differ).  norm: of every head's D channels ahead of the rotation. */
+ * differ).  norm: of every head's D channels ahead of the rotation.  Of the
+ * attention's size limits none holds here: L <= 2^27, B * L < 2^31, B and H below
+ * 2^16, strides up to 2^40 elements. */
 svd_status svd_rope_forward(const svd_rope_desc* rope, const float* table, int32_t norm, float eps,
                             const svd_rope_tensor* tensors, int32_t n_tensors, void* hip_stream);
 

@@ -3,10 +3,10 @@
 #include <cmath>
 #include <cstddef>
 #include <cstdint>
+#include <initializer_list>
 
 #include "layer_index.h"
 #include "layer_ops.h"
-#include "plan.h"
 #include "sparse_vdit.h"
 
 namespace {
@@ -129,23 +129,29 @@ svd_status check_rope(const svd_rope_desc& r) {
   return SVD_OK;
 }
 
+// Heads of q or k: the rotary kernels form offsets in 64 bits, so the limits of the attention's tensors do not hold here.
+constexpr int32_t kMaxRopeRows = 1 << 27;   // a launch has less than 2^32 threads an axis
 svd_status check_heads(const svd_tensor_desc* t, int32_t B, int32_t L, int32_t D) {
   if (!t) return SVD_ERR_NULL;
-  if (t->B != B || t->L != L || t->D != D || t->H < 1 || t->H > 65535) return SVD_ERR_SHAPE;
-  return svd::validate_desc(t);
+  if (t->B < 1 || t->L < 1 || t->H < 1 || t->H > 65535 || (t->D != 64 && t->D != 128)) return SVD_ERR_SHAPE;
+  if (t->B != B || t->L != L || t->D != D) return SVD_ERR_SHAPE;
+  if (t->stride_l < t->D || t->stride_b < 1 || t->stride_h < 1) return SVD_ERR_SHAPE;
+  if (t->stride_l > kMaxStride || t->stride_b > kMaxStride || t->stride_h > kMaxStride) return SVD_ERR_SHAPE;
+  if (t->stride_b % 8 || t->stride_h % 8 || t->stride_l % 8) return SVD_ERR_ALIGN;
+  return SVD_OK;
 }
 
 svd_status check_rope_call(const svd_rope_desc* rope, const float* table, int32_t norm, float eps, int32_t n,
                            const svd_tensor_desc* d, svd::RopeLaunch* p) {
   if (!d) return SVD_ERR_NULL;
   if (svd_status st = check_rope(*rope)) return st;
-  if (svd_status st = svd::validate_desc(d)) return st;
+  if (svd_status st = check_heads(d, d->B, d->L, d->D)) return st;
   if (2 * (rope->pairs_t + rope->pairs_h + rope->pairs_w) > d->D) return SVD_ERR_PARAMS;
   if (!table && rope_entries(*rope) > 0) return SVD_ERR_NULL;
   if (!aligned16(table)) return SVD_ERR_ALIGN;
   if (norm < SVD_NORM_NONE || norm > SVD_NORM_RMS) return SVD_ERR_PARAMS;
   if (norm != SVD_NORM_NONE && (!(eps > 0.f) || !std::isfinite(eps))) return SVD_ERR_PARAMS;
-  if (d->B > 65535 || static_cast<int64_t>(d->B) * d->L > INT32_MAX) return SVD_ERR_UNSUPPORTED;
+  if (d->B > 65535 || d->L > kMaxRopeRows || static_cast<int64_t>(d->B) * d->L > INT32_MAX) return SVD_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(rope->row_offset) + d->L > INT32_MAX) return SVD_ERR_UNSUPPORTED;
   p->r = *rope;
   p->table = table;
