@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) rope_backward_kernel(const RopeLaunc
     }
   }
   if (!p.partial) return;
-  __shared__ float sums[TOKENS][2][D];
+  __shared__ __attribute__((aligned(16))) float sums[TOKENS][2][D];
   P::store(sums[threadIdx.x / LANES][0], c, D, dw);
   P::store(sums[threadIdx.x / LANES][1], c, D, db);
   __syncthreads();
