@@ -822,6 +822,7 @@ def svd_rope_forward(rope: RopeDesc, table, tensors, norm="none", eps=1e-6, stre
 
 
 def svd_rope_backward_workspace_bytes(B, L, D) -> int:
+    _within_31_bits(B | L | D)
     n = C.c_size_t()
     _check(lib().svd_rope_backward_workspace_bytes(B, L, D, C.byref(n)), "svd_rope_backward_workspace_bytes")
     return n.value
