@@ -492,7 +492,7 @@ svd_status svd_probe_copy(const void* src, void* dst, size_t bytes, void* hip_st
  * enqueues one to three kernels and can be captured.  Sums, norms and rotations are
  * held in fp32 and rounded once, to the type of the output.  Vectors (weights,
  * gates, biases and their gradients) are fp32. */
-enum { SVD_BF16 = 0, SVD_F32 = 1, SVD_E4M3 = 2 };   /* element types */
+enum { SVD_BF16 = 0, SVD_F32 = 1 };   /* element types */
 enum { SVD_NORM_NONE = 0, SVD_NORM_LAYER = 1, SVD_NORM_RMS = 2 };
 
 /* B x L rows of C channels: element strides of the two outer axes, channels
