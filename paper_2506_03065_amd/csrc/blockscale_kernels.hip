@@ -31,19 +31,17 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 // ---- quantisation ----
 
-// Work-group: 32 rows by BLOCKS blocks of 128 columns; a wave 8 rows, 16 lanes a block, four or two rows at once where
-// the rows are of one or two blocks (300,000 x 128 bf16: 17.5 us against 43; 75,600 x 256: 10.7 against 16.5).  The scale bytes of a block's 32 rows go out together.
-constexpr int kQuantRows = 32;
+// Work-group: 32 rows by BLOCKS blocks of 128 columns.  The scale bytes of a block's 32 rows go out together.
 template <typename T, int BLOCKS>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(const QuantLaunch p) {
-  constexpr int ROWS = 4 / BLOCKS;   // of a wave at once
+  constexpr int ROWS = quant_rows_at_once(BLOCKS);
   __shared__ __attribute__((aligned(16))) uint8_t bytes[BLOCKS][kQuantRows];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = (lane >> 4) % BLOCKS, first = wave * 8 + (lane >> 4) / BLOCKS;
-  const int r0 = blockIdx.x * kQuantRows, block = blockIdx.y * BLOCKS + mine, c = block * 128 + (lane & 15) * 8;
+  const QuantAt at = quant_at(threadIdx.x, BLOCKS);
+  const int r0 = blockIdx.x * kQuantRows, c = (blockIdx.y * BLOCKS + at.block) * 128 + at.column;
   const int c16 = (p.C + 15) / 16 * 16;
 #pragma unroll
   for (int i = 0; i < 8 / ROWS; ++i) {
-    const int k = first + i * ROWS, row = r0 + k;
+    const int k = at.row + i * ROWS, row = r0 + k;
     const T* src = static_cast<const T*>(p.src) + (int64_t)row * p.src_stride + c;
     f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
     if (row < p.R && c + 8 <= p.C) {
@@ -65,7 +63,7 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(const QuantLaunch p)
                        (unsigned)pack_e4m3(v[4] * f, v[5] * f, v[6] * f, v[7] * f)};
       *reinterpret_cast<u32x2*>(p.dst + (int64_t)row * p.dst_stride + c) = w;
     }
-    if ((lane & 15) == 0) bytes[mine][k] = (uint8_t)byte;
+    if ((threadIdx.x & 15) == 0) bytes[at.block][k] = (uint8_t)byte;
   }
   __syncthreads();
   const int b = threadIdx.x / kQuantRows, k = threadIdx.x % kQuantRows;
@@ -82,7 +80,8 @@ __global__ void __launch_bounds__(256) quantise_columns_kernel(const QuantLaunch
   const int r0 = blockIdx.y * 128, c0 = blockIdx.x * 64;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int k = i * 32 + threadIdx.x / 8, c = (threadIdx.x & 7) * 8, row = r0 + k;
+    const QuantPlace at = quant_read_at(threadIdx.x, i);
+    const int k = at.row, c = at.column, row = r0 + k;
     const T* src = static_cast<const T*>(p.src) + (int64_t)row * p.src_stride + c0 + c;
     f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
     if (row < p.R && c0 + c + 8 <= p.C) {
@@ -98,12 +97,13 @@ __global__ void __launch_bounds__(256) quantise_columns_kernel(const QuantLaunch
     for (int j = 0; j < 8; ++j) tile[k * PAD + c + j] = v[j];
   }
   __syncthreads();
-  const int col = threadIdx.x >> 2, part = threadIdx.x & 3;
+  const QuantPlace at = quant_write_at(threadIdx.x);
+  const int col = at.column, part = threadIdx.x & 3;
   float v[32];
   int top = 0;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    v[i] = tile[(part * 32 + i) * PAD + col];
+    v[i] = tile[(at.row + i) * PAD + col];
     top = max(top, magnitude(v[i]));
   }
   top = max(top, dpp<kXor1>(top));
@@ -112,14 +112,14 @@ __global__ void __launch_bounds__(256) quantise_columns_kernel(const QuantLaunch
   const float f = scale_inverse(byte);
   if (c0 + col >= p.C) return;
   const int r16 = (p.R + 15) / 16 * 16;
-  uint8_t* dst = p.dst + (int64_t)(c0 + col) * p.dst_stride + r0 + part * 32;
+  uint8_t* dst = p.dst + (int64_t)(c0 + col) * p.dst_stride + r0 + at.row;
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     u32x4 w;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       w[j] = (unsigned)pack_e4m3(v[16 * q + 4 * j] * f, v[16 * q + 4 * j + 1] * f, v[16 * q + 4 * j + 2] * f, v[16 * q + 4 * j + 3] * f);
-    if (r0 + part * 32 + 16 * q < r16) *reinterpret_cast<u32x4*>(dst + 16 * q) = w;
+    if (r0 + at.row + 16 * q < r16) *reinterpret_cast<u32x4*>(dst + 16 * q) = w;
   }
   if (part == 0) p.scales[(int64_t)blockIdx.y * p.scale_stride + c0 + col] = (uint8_t)byte;
 }
@@ -472,7 +472,7 @@ void launch_tiles(const MatmulLaunch& p, int tiles, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_quantise_rows(const QuantLaunch& p, hipStream_t stream) {
-  const int blocks = p.C <= 128 ? 1 : p.C <= 256 ? 2 : 4;
+  const int blocks = quant_blocks(p.C);
   const dim3 grid((p.R + kQuantRows - 1) / kQuantRows, (p.C + blocks * 128 - 1) / (blocks * 128));
   auto launch = [&](auto type) {
     using T = decltype(type);

@@ -76,7 +76,59 @@ constexpr NormShape norm_shape(int C, int group) {
   return {0, pieces, (C / 8 + 64 * pieces - 1) / (64 * pieces) * 64, 1};
 }
 
+// ---- sums of the groups ----
+
+// Group of a work-group of the joining kernel: `y` is at most 32,768 of a launch, `z` the rest.
+constexpr int kJoinRow = 32768;
+constexpr int join_at(int y, int z) { return y + z * kJoinRow; }
+// Threads a channel of it: as many as a group has chunks for (30,000 x 512 in groups of one row: 470 us of four threads a channel, 201 of one).
+constexpr int join_lanes(const RowChunks& c) {
+  const int chunks = c.group_chunks > c.first_chunks ? c.group_chunks : c.first_chunks;
+  return chunks > 64 ? 32 : chunks > 4 ? 8 : 1;
+}
+// Number u of the eight that a thread of a column takes in a step from `i` on (n or more: none).
+constexpr int kSumAhead = 8;
+constexpr int sum_at(int i, int u, int lanes) { return i + u * lanes; }
+
 // ---- rotary positions ----
+
+constexpr int kRopeThreads = 256;
+constexpr int rope_tokens(int D) { return kRopeThreads / (D / 8); }   // of a work-group: 8 channels of one to a thread
+constexpr int rope_blocks(int L, int D) { return (L + rope_tokens(D) - 1) / rope_tokens(D); }
+
+struct HeadRange {
+  int first, last;   // [first, last)
+};
+constexpr HeadRange heads_of_part(int H, int splits, int part) {
+  const int per = (H + splits - 1) / splits, first = part * per;
+  return {first, first + per < H ? first + per : H};
+}
+
+// Parts of the heads, forward: few tokens share the heads out, until the chip has 2,048 work-groups or a thread one head.
+constexpr int rope_forward_splits(int L, int B, int D, int n, int heads) {
+  const int64_t splits = 2048 / ((int64_t)rope_blocks(L, D) * B * n);
+  return (int)(splits < 1 ? 1 : splits > heads ? heads : splits);
+}
+
+// Backward: a unit is a block of tokens and a part of the heads; a work-group walks units in steps of the launch, so that the partial sums
+// stay few.  Parts so that every work-group has 4 units or more: the last, partly filled round is then little of the whole.
+// (48 heads of 64 x 21,825, q and k: 170 us for 4, 173 for 8, 177 for 16, 204 for a unit of all heads.)
+constexpr int kRopePartials = 512;   // work-groups of a tensor, at most, that leave a partial sum
+struct RopeWalk {
+  int splits, groups;
+};
+constexpr RopeWalk rope_walk(int L, int B, int D, int heads) {
+  const int64_t blocks = (int64_t)B * rope_blocks(L, D), want = (4 * kRopePartials + blocks - 1) / blocks;
+  const int splits = (int)(want > heads ? heads : want);
+  return {splits, (int)(blocks * splits < kRopePartials ? blocks * splits : kRopePartials)};
+}
+struct RopeUnit {
+  int b, block, part;
+};
+constexpr RopeUnit rope_unit(int64_t i, int blocks, int splits) {
+  const int at = (int)(i / splits);
+  return {at / blocks, at % blocks, (int)(i % splits)};
+}
 
 struct Place {
   bool video;
@@ -89,6 +141,27 @@ constexpr Place place_of(int token, int frames, int height, int width, bool posi
   const int pos = position_major ? token / frames : token % N;
   return {true, position_major ? token % frames : token / N, pos / width, pos % width};
 }
+
+// ---- blocks of 128 ----
+
+// By rows: a work-group takes 32 rows of `blocks` blocks, a wave 8 rows, 16 lanes a block, four or two rows at once where the rows are of
+// one or two blocks (300,000 x 128 bf16: 17.5 us against 43; 75,600 x 256: 10.7 against 16.5).
+constexpr int kQuantRows = 32;
+constexpr int quant_blocks(int C) { return C <= 128 ? 1 : C <= 256 ? 2 : 4; }
+constexpr int quant_rows_at_once(int blocks) { return 4 / blocks; }   // of a wave
+struct QuantAt {
+  int block, row, column;   // of the work-group; first row of the thread, its further ones quant_rows_at_once apart; of the block
+};
+constexpr QuantAt quant_at(int thread, int blocks) {
+  const int quarter = (thread & 63) >> 4;
+  return {quarter % blocks, (thread >> 6) * 8 + quarter / blocks, (thread & 15) * 8};
+}
+// By columns: 128 rows of 64 columns, read in four steps of 32 rows, 8 columns a thread; then a thread has 32 rows of a column.
+struct QuantPlace {
+  int row, column;
+};
+constexpr QuantPlace quant_read_at(int thread, int step) { return {step * 32 + thread / 8, (thread & 7) * 8}; }
+constexpr QuantPlace quant_write_at(int thread) { return {(thread & 3) * 32, thread >> 2}; }
 
 // ---- block-scaled products ----
 

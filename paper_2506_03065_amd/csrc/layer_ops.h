@@ -57,7 +57,6 @@ struct RopeLaunch {
   RopeTensor t[2];
   float* partial;   // [n][work-groups][2][D]
 };
-constexpr int kRopePartials = 512;   // work-groups of a tensor, at most, that leave a partial sum in a backward pass
 hipError_t launch_rope_table(const svd_rope_desc& r, double base, const double start[3], const double step[3], float* table,
                              hipStream_t stream);
 hipError_t launch_rope_forward(const RopeLaunch& p, hipStream_t stream);

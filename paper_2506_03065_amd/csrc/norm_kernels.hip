@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(NJ == 1 || LANES ? 256 : 512) norm_backward_ke
 template <int LANES>
 __global__ void __launch_bounds__(LANES == 1 ? 256 : 32 * LANES) norm_group_kernel(const NormLaunch p) {
   constexpr int COLUMNS = LANES == 1 ? 256 : 32;
-  const int column = threadIdx.x % COLUMNS, c = blockIdx.x * COLUMNS + column, bg = blockIdx.y + blockIdx.z * 32768;
+  const int column = threadIdx.x % COLUMNS, c = blockIdx.x * COLUMNS + column, bg = join_at(blockIdx.y, blockIdx.z);
   if (bg >= p.B * p.ch.groups) return;
   const int b = bg / p.ch.groups, g = bg % p.ch.groups;
   const ChunkRange chunks = chunks_of(p.ch, g);
@@ -489,11 +489,10 @@ hipError_t launch_norm_backward(const NormLaunch& p, hipStream_t stream) {
   SVD_NORM_LAUNCH(norm_backward_kernel);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.partial) return e;
   const int n = p.B * p.ch.groups, columns = (p.C + 31) / 32;
-  dim3 groups(columns, n < 32768 ? n : 32768, (n + 32767) / 32768);
-  // as many threads a channel as a group has chunks for (30,000 x 512 in groups of one row: 470 us of four threads a channel, 201 of one)
-  const int chunks = p.ch.group_chunks > p.ch.first_chunks ? p.ch.group_chunks : p.ch.first_chunks;
-  if (chunks > 64) hipLaunchKernelGGL(norm_group_kernel<32>, groups, dim3(1024), 0, stream, p);
-  else if (chunks > 4) hipLaunchKernelGGL(norm_group_kernel<8>, groups, dim3(256), 0, stream, p);
+  dim3 groups(columns, n < kJoinRow ? n : kJoinRow, (n + kJoinRow - 1) / kJoinRow);
+  const int lanes = join_lanes(p.ch);
+  if (lanes == 32) hipLaunchKernelGGL(norm_group_kernel<32>, groups, dim3(1024), 0, stream, p);
+  else if (lanes == 8) hipLaunchKernelGGL(norm_group_kernel<8>, groups, dim3(256), 0, stream, p);
   else {
     groups.x = (p.C + 255) / 256;
     hipLaunchKernelGGL(norm_group_kernel<1>, groups, dim3(256), 0, stream, p);

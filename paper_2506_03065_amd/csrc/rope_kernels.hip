@@ -11,7 +11,7 @@
 namespace svd {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRopeThreads;
 
 // A thread's 8 channels: 8 in a row (pairs of neighbours), or 4 from either half.
 template <bool HALVES>
@@ -115,13 +115,13 @@ __global__ void __launch_bounds__(kThreads) rope_forward_kernel(const RopeLaunch
   const RopeTensor& t = p.t[blockIdx.z / splits];
   const int c = threadIdx.x % LANES, l = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES, b = blockIdx.y;
   if (l >= p.L) return;
-  const int part = blockIdx.z % splits, per = (t.H + splits - 1) / splits, h0 = part * per, h1 = min(h0 + per, t.H);
+  const HeadRange heads = heads_of_part(t.H, splits, blockIdx.z % splits);
   const Angles a = angles_of(p, l, c);
   const f32x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   const f32x8 w = t.weight ? P::load(t.weight, c, D) : zero + 1.f, bias = t.bias ? P::load(t.bias, c, D) : zero;
   const __bf16* x = t.x + (int64_t)b * t.x_b + (int64_t)l * t.x_l;
   __bf16* o = t.out + (int64_t)b * t.o_b + (int64_t)l * t.o_l;
-  for (int h = h0; h < h1; ++h) {
+  for (int h = heads.first; h < heads.last; ++h) {
     f32x8 v = __builtin_convertvector(P::raw(x + (int64_t)h * t.x_h, c, D), f32x8);
     if (p.norm != SVD_NORM_NONE) {
       normalise<LANES>(v, p.norm, p.eps);
@@ -132,8 +132,7 @@ __global__ void __launch_bounds__(kThreads) rope_forward_kernel(const RopeLaunch
 }
 
 // d = turned back dout; dweight = sum d n, dbias = sum d over all rows; dx = r (dn - mean(dn) - n mean(dn n)), dn = d w.
-// A unit is a block of tokens and a part of the heads; a work-group walks units in steps of kPartials, so that the partial sums
-// stay few.  The next head's loads are in flight while a head is worked on.
+// A work-group walks units of a block of tokens and a part of the heads.  The next head's loads are in flight while a head is worked on.
 template <int D, bool HALVES>
 __global__ void __launch_bounds__(kThreads) rope_backward_kernel(const RopeLaunch p, const int splits) {
   constexpr int LANES = D / 8, TOKENS = kThreads / LANES;
@@ -145,11 +144,13 @@ __global__ void __launch_bounds__(kThreads) rope_backward_kernel(const RopeLaunc
   const f32x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   const f32x8 w = t.weight ? P::load(t.weight, c, D) : zero + 1.f;
   f32x8 dw = zero, db = zero;
-  const int blocks = (p.L + TOKENS - 1) / TOKENS, per = (t.H + splits - 1) / splits;
+  const int blocks = rope_blocks(p.L, D);
   const int64_t units = (int64_t)blocks * p.B * splits;
   for (int64_t i = blockIdx.x; i < units; i += gridDim.x) {
-    const int part = (int)(i % splits), block = (int)(i / splits), b = block / blocks, l = (block % blocks) * TOKENS + threadIdx.x / LANES;
-    const int h0 = part * per, h1 = min(h0 + per, t.H);
+    const RopeUnit unit = rope_unit(i, blocks, splits);
+    const int b = unit.b, l = unit.block * TOKENS + threadIdx.x / LANES;
+    const HeadRange heads = heads_of_part(t.H, splits, unit.part);
+    const int h0 = heads.first, h1 = heads.last;
     if (l >= p.L || h0 >= h1) continue;
     const __bf16* x = normed ? t.x + (int64_t)b * t.x_b + (int64_t)l * t.x_l : nullptr;
     const __bf16* g = t.dout + (int64_t)b * t.d_b + (int64_t)l * t.d_l;
@@ -213,6 +214,8 @@ __global__ void __launch_bounds__(kThreads) rope_table_kernel(const TableArgs a,
   table[i] = make_float2((float)cos(angle), (float)sin(angle));
 }
 
+int most_heads(const RopeLaunch& p) { return p.n == 2 && p.t[1].H > p.t[0].H ? p.t[1].H : p.t[0].H; }
+
 }  // namespace
 
 hipError_t launch_rope_table(const svd_rope_desc& r, double base, const double start[3], const double step[3], float* table,
@@ -225,14 +228,10 @@ hipError_t launch_rope_table(const svd_rope_desc& r, double base, const double s
 }
 
 hipError_t launch_rope_forward(const RopeLaunch& p, hipStream_t stream) {
-  const int tokens = kThreads / (p.D / 8), blocks = (p.L + tokens - 1) / tokens;
-  const int heads = p.n == 2 && p.t[1].H > p.t[0].H ? p.t[1].H : p.t[0].H;
-  // Few tokens: the heads are shared out, until the chip has 2,048 work-groups or a thread one head.
-  int64_t splits = 2048 / ((int64_t)blocks * p.B * p.n);
-  splits = splits < 1 ? 1 : splits > heads ? heads : splits;
-  const dim3 grid(blocks, p.B, (unsigned)(p.n * splits));
+  const int splits = rope_forward_splits(p.L, p.B, p.D, p.n, most_heads(p));
+  const dim3 grid(rope_blocks(p.L, p.D), p.B, (unsigned)(p.n * splits));
   const bool halves = p.r.pairing == SVD_ROPE_HALVES;
-#define SVD_ROPE_LAUNCH(D, H) hipLaunchKernelGGL((rope_forward_kernel<D, H>), grid, dim3(kThreads), 0, stream, p, (int)splits)
+#define SVD_ROPE_LAUNCH(D, H) hipLaunchKernelGGL((rope_forward_kernel<D, H>), grid, dim3(kThreads), 0, stream, p, splits)
   if (p.D == 64) {
     if (halves) SVD_ROPE_LAUNCH(64, true);
     else SVD_ROPE_LAUNCH(64, false);
@@ -245,18 +244,10 @@ hipError_t launch_rope_forward(const RopeLaunch& p, hipStream_t stream) {
 }
 
 hipError_t launch_rope_backward(const RopeLaunch& p, hipStream_t stream) {
-  const int tokens = kThreads / (p.D / 8);
-  const int heads = p.n == 2 && p.t[1].H > p.t[0].H ? p.t[1].H : p.t[0].H;
-  const int64_t blocks = (int64_t)p.B * ((p.L + tokens - 1) / tokens);
-  // Parts of the heads so that every work-group has 4 units or more: the last, partly filled round is then little of the whole.
-  // (48 heads of 64 x 21,825, q and k: 170 us for 4, 173 for 8, 177 for 16, 204 for a unit of all heads.)
-  int64_t splits = (4 * kRopePartials + blocks - 1) / blocks;
-  splits = splits > heads ? heads : splits;
-  const int64_t units = blocks * splits;
-  const int groups = (int)(units < kRopePartials ? units : kRopePartials);
-  const dim3 grid(groups, p.n);
+  const RopeWalk walk = rope_walk(p.L, p.B, p.D, most_heads(p));
+  const dim3 grid(walk.groups, p.n);
   const bool halves = p.r.pairing == SVD_ROPE_HALVES;
-#define SVD_ROPE_LAUNCH(D, H) hipLaunchKernelGGL((rope_backward_kernel<D, H>), grid, dim3(kThreads), 0, stream, p, (int)splits)
+#define SVD_ROPE_LAUNCH(D, H) hipLaunchKernelGGL((rope_backward_kernel<D, H>), grid, dim3(kThreads), 0, stream, p, walk.splits)
   if (p.D == 64) {
     if (halves) SVD_ROPE_LAUNCH(64, true);
     else SVD_ROPE_LAUNCH(64, false);
@@ -266,7 +257,7 @@ hipError_t launch_rope_backward(const RopeLaunch& p, hipStream_t stream) {
   }
 #undef SVD_ROPE_LAUNCH
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.partial) return e;
-  hipLaunchKernelGGL(rope_weight_kernel, dim3(p.D / 32, 2 * p.n), dim3(1024), 0, stream, p, groups);
+  hipLaunchKernelGGL(rope_weight_kernel, dim3(p.D / 32, 2 * p.n), dim3(1024), 0, stream, p, walk.groups);
   return hipGetLastError();
 }
 

@@ -5,6 +5,8 @@
 
 #include <cstdint>
 
+#include "layer_index.h"
+
 namespace svd {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -91,7 +93,7 @@ __device__ __forceinline__ void store8(float* p, const f32x8 v) {
 // (`on` false) add nothing.
 template <int LANES, int NV>
 __device__ __forceinline__ double column_sums(const float* in, int64_t next, int64_t stride, int n, bool on, double (*slots)[LANES][32]) {
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = kSumAhead;
   const int lane = threadIdx.x / 32, column = threadIdx.x % 32;
   double s[NV] = {};
   if (on)
@@ -100,11 +102,11 @@ __device__ __forceinline__ double column_sums(const float* in, int64_t next, int
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) v[u][k] = in[(int64_t)min(i + u * LANES, n - 1) * stride + k * next];
+        for (int k = 0; k < NV; ++k) v[u][k] = in[(int64_t)min(sum_at(i, u, LANES), n - 1) * stride + k * next];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) s[k] += i + u * LANES < n ? (double)v[u][k] : 0.0;
+        for (int k = 0; k < NV; ++k) s[k] += sum_at(i, u, LANES) < n ? (double)v[u][k] : 0.0;
     }
 #pragma unroll
   for (int k = 0; k < NV; ++k) slots[k][lane][column] = s[k];

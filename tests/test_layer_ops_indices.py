@@ -18,7 +18,7 @@ def indices(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("part", ["rows"])
+@pytest.mark.parametrize("part", ["rows", "rope", "quantise", "joins"])
 def test_everything_once(indices, part):
     res = subprocess.run([indices, part], capture_output=True, text=True, timeout=600, env=dict(os.environ, UBSAN_OPTIONS="print_stacktrace=1"))
     assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-4000:]
