@@ -1,7 +1,8 @@
-// Host models of the kernel launches behind layer_ops.h.  No arithmetic on values: for every work-group a launch would start, the
-// model walks the kernel's index arithmetic (layer_index.h, which the kernels share) and touches, on the host, every row, vector,
-// table entry, partial sum, tile and scale byte that the kernel would address.  All of that memory is exact-size heap memory of
-// the test, so an index that leaves its buffer is an AddressSanitizer report and a violation.
+// Host models of the kernel launches behind layer_ops.h.  No arithmetic on values: the models touch, on the host, every row, vector,
+// table entry, partial sum, tile and scale byte that a launch would address, the norms' and the product's through the kernels' own index
+// arithmetic (layer_index.h), work-group by work-group.  (That of the rotary kernels, of the quantisation and of the joins of sums is
+// walked in layer_indices.cpp.)  All of that memory is exact-size heap memory of the test, so an index that leaves its buffer is an
+// AddressSanitizer report and a violation.
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
@@ -9,17 +10,8 @@
 
 #include "hip_stub.h"
 #include "layer_ops.h"
-#include "plan.h"
 
 namespace svd {
-
-// as in pattern_compiler.cpp, whose other code these calls do not need
-svd_status validate_desc(const svd_tensor_desc* d) {
-  if (!d) return SVD_ERR_NULL;
-  if (d->B < 1 || d->H < 1 || d->L < 1 || (d->D != 64 && d->D != 128) || d->stride_l < d->D || d->stride_b < 1 || d->stride_h < 1) return SVD_ERR_SHAPE;
-  if (d->stride_b % 8 || d->stride_h % 8 || d->stride_l % 8) return SVD_ERR_ALIGN;
-  return SVD_OK;
-}
 
 namespace {
 
