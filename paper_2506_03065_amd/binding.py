@@ -853,7 +853,7 @@ def svd_rope_backward(rope: RopeDesc, table, tensors, norm="none", eps=1e-6, wor
 
 
 def _scale_stride(scales):
-    return scales.stride(0) if scales.shape[0] > 1 else scales.shape[-1]
+    return scales.stride(0) if scales.shape[0] > 1 else -(-scales.shape[-1] // 16) * 16   # of one block it says nothing
 
 
 def blockscale_empty(rows, columns, device):
