@@ -584,6 +584,7 @@ def svd_search_layer(q, k, v, params_by_mode, lam, eps, out, workspace, stream=N
 
 
 # ---- operators around the attention of a layer ----
+# Results go into the tensors that are passed; torch.autograd records none of these calls, the backward passes are calls of their own.
 
 _NORMS = {"none": 0, "layer": 1, "rms": 2}
 _PAIRINGS = {"adjacent": 0, "halves": 1}
@@ -860,7 +861,7 @@ def blockscale_empty(rows, columns, device):
     """Memory of a matrix in E4M3 with a scale for each block of 128 columns: (float8_e4m3fn [rows, columns], rows a multiple of 16
     bytes apart, long ones in whole lines of 128; uint8 [ceil(columns / 128), rows rounded up to 16])."""
     import torch
-    # A block of a row is then one line of memory, not parts of two (7,680 x 1,920 x 11,881: 155 -> 136 us), for at most an eighth more.
+    # A block of a row is then one line of memory, not parts of two (7,680 x 1,920 x 11,881: 157 -> 148 us), for at most an eighth more.
     line = 128 if columns >= 1024 else 16
     values = torch.empty(rows, -(-columns // line) * line, device=device, dtype=torch.float8_e4m3fn)
     return values[:, :columns], torch.empty(-(-columns // 128), -(-rows // 16) * 16, device=device, dtype=torch.uint8)

@@ -190,14 +190,15 @@ constexpr int swizzle(int row, int tiles) { return (row / tiles) & 15; }
 // The last for up to 64 rows, or where the chip's 256 units take the product in one round that way (two rounds, if K is long).
 // Otherwise the rounds decide: one of large tiles counts 100, one of 512 small tiles 69, the rest of at most 256 small tiles 45.
 // The large tiles behind the last full round go in quarters, as small tiles in a launch of its own (counted 12), if K is not
-// short and that is to save a thirtieth part: over many rounds the units part anyway. us whole / cut: 11,881 x 1,920 x 7,680:
-// 159 / 152; 24,000 x 1,000 x 4,096: 93 / 90; 9,107 x 6,144 x 2,048: 113 / 110; 20,000 x 2,048 x 2,048: 87 / 84; not so
-// 11,881 x 1,920 x 1,024: 33.4 / 34.5; 75,600 x 5,120 x 5,120: 1,557 / 1,573.
-// us for 256 / 128 / 64:
-// 75,600 x 5,120 x 5,120: 1,555 / 1,902 / -;  9,107 x 6,144 x 2,048: 114 / 121 / -;  11,881 x 1,920 x 7,680: 159 / 165 / -;
-// 7,680 x 1,920 x 11,881: 148 / 172 / 301;  6,000 x 3,300 x 4,096: 120 / 105 / 208;  1,920 x 1,920 x 30,000: 253 / 146 / 179;
-// 800 x 1,536 x 8,192: 71 / 40.1 / 31.2;  800 x 1,536 x 2,048: 22.1 / 10.9 / 12.6;  1,000 x 1,920 x 1,920: 24.5 / 13.0 / 13.9;
-// 300 x 1,920 x 1,920: 23.0 / 10.1 / 7.5;  128 x 5,120 x 5,120: 50 / 29.7 / 13.3;  2 x 30,720 x 5,120: - / 41.5 / 33.8.
+// short and that is to save a thirtieth part: over many rounds the units part anyway. us whole / cut, in turn on one card:
+// 11,881 x 1,920 x 7,680: 167 / 156; 24,000 x 1,000 x 4,096: 93 / 88; 9,107 x 6,144 x 2,048: 111 / 108; 20,000 x 2,048 x 2,048: 85 / 82;
+// not so 11,881 x 1,920 x 1,024: 33.1 / 33.7; 75,600 x 5,120 x 5,120: 1,556 / 1,578.
+// us for 256 / 128 / 64, on the same card (another takes up to 6 % more or less):
+// 75,600 x 5,120 x 5,120: 1,556 / 1,886 / 3,958;  9,107 x 6,144 x 2,048: 111 / 119 / 307;  11,881 x 1,920 x 7,680: 167 / 163 / 327;
+// 7,680 x 1,920 x 11,881: 146 / 162 / 298;  6,000 x 3,300 x 4,096: 120 / 107 / 197;  1,920 x 1,920 x 30,000: 254 / 148 / 178;
+// 800 x 1,536 x 8,192: 71 / 39.7 / 29.7;  800 x 1,536 x 2,048: 23.5 / 13.7 / 13.8;  1,000 x 1,920 x 1,920: 22.7 / 13.9 / 13.8;
+// 300 x 1,920 x 1,920: 20.8 / 10.8 / 7.4;  128 x 5,120 x 5,120: 46.7 / 29.9 / 13.3;  17 x 4,096 x 4,096: 36.4 / 20.8 / 9.8;
+// 2 x 30,720 x 5,120: 63 / 42.7 / 32.6.
 enum { FORM_64 = 0, FORM_128 = 1, FORM_256 = 2 };
 struct MatmulPlan {
   int form;
