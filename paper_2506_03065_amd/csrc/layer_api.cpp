@@ -136,7 +136,7 @@ svd_status check_heads(const svd_tensor_desc* t, int32_t B, int32_t L, int32_t D
   if (t->B < 1 || t->L < 1 || t->H < 1 || t->H > 65535 || (t->D != 64 && t->D != 128)) return SVD_ERR_SHAPE;
   if (t->B != B || t->L != L || t->D != D) return SVD_ERR_SHAPE;
   if (t->stride_l < t->D || t->stride_b < 1 || t->stride_h < 1) return SVD_ERR_SHAPE;
-  if (t->stride_l > kMaxStride || t->stride_b > kMaxStride || t->stride_h > kMaxStride) return SVD_ERR_SHAPE;
+  if ((t->L > 1 && t->stride_l > kMaxStride) || (t->B > 1 && t->stride_b > kMaxStride) || (t->H > 1 && t->stride_h > kMaxStride)) return SVD_ERR_SHAPE;
   if (t->stride_b % 8 || t->stride_h % 8 || t->stride_l % 8) return SVD_ERR_ALIGN;
   return SVD_OK;
 }

@@ -49,6 +49,7 @@ int main() {
   rope(SVD_ERR_UNSUPPORTED, "one more", {1, 1, (1 << 27) + 1, 128, (int64_t)1 << 35, 128, 128});
   rope(SVD_ERR_UNSUPPORTED, "rows of all entries", {16, 1, 1 << 27, 64, 64, 64, 64});
   rope(SVD_ERR_SHAPE, "a stride past 2^40", {1, 2, 100, 64, 64, ((int64_t)1 << 40) + 8, 64});
+  rope(SVD_OK, "an axis of length 1 needs no stride", {1, 1, 1, 64, (int64_t)1 << 62, (int64_t)1 << 62, (int64_t)1 << 62});
   rope(SVD_ERR_SHAPE, "rows over one another", {1, 1, 100, 64, 6400, 6400, 56});
   rope(SVD_ERR_SHAPE, "heads over one another", {1, 2, 100, 64, 6400, 0, 128});
   rope(SVD_ERR_SHAPE, "more heads than a launch has", {1, 65536, 1, 64, 64 * 65536, 64, 64 * 65536});

@@ -9,6 +9,12 @@ DEV = "cuda:0"
 BF = torch.bfloat16
 
 
+@pytest.fixture(autouse=True)
+def memory_given_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("L", [2 ** 31 - 1, 2 ** 31 - 8])
 def test_norms_of_the_most_rows(L):
     """As many rows as a call takes, of 8 channels (34 GB a tensor): the last rows against the same rows alone, and a sum over the
